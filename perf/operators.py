@@ -233,12 +233,12 @@ def _prepare_sample(case, g):
     per = 4 if case["dtype"] == "f32" else 8
     ld = vocab + case["pad"]
     ld += -ld % per
-    # logits as a language model's: a broad body, and 200 entries that stand out of it by up to 10 to
-    # 16, by row: most rows' mass is on some tens of entries, some rows' reaches far into the body
+    # logits as a language model's: a broad body and some hundred entries that stand out, by row
     z = torch.empty((rows, ld), device="cuda").normal_(0.0, 2.0, generator=g)
     at = torch.randint(0, vocab, (rows, 200), device="cuda", generator=g)
-    high = 10.0 + 6.0 * torch.rand(rows, 1, device="cuda", generator=g)
-    z.scatter_add_(1, at, high * (0.3 + 0.7 * torch.rand(rows, 200, device="cuda", generator=g)))
+    z.scatter_add_(1, at, 3.0 + 4.0 * torch.rand(rows, 200, device="cuda", generator=g))
+    best = torch.randint(0, vocab, (rows, 1), device="cuda", generator=g)
+    z.scatter_add_(1, best, 9.0 + 3.0 * torch.rand(rows, 1, device="cuda", generator=g))
     s = dict(case=case, logits=z.to(_dtype(case)))
     del z
     s["noise"] = torch.empty((rows, vocab + -vocab % 4), device="cuda").exponential_(generator=g)
