@@ -664,7 +664,7 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
             __syncthreads();
             // 16 threads per row
             const int row = tid >> 4, r = at.rt * Rows + t * 16 + row;
-            if (r >= n_rows) continue;  // not past a barrier: those of the next tile are met by all
+            if (r >= n_rows) continue;  // not past a barrier: those of the next tile and of the item's end are met by all
             float m = s_m[0][row], sum = 0.0f, f[kWaves];
 #pragma unroll
             for (int i = 1; i < kWaves; ++i) m = fmaxf(m, s_m[i][row]);
@@ -703,6 +703,7 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
                 }
             }
         }
+        __syncthreads();  // `buf` has been read: the next item's keys and values go there
         if (at.same_item(to)) break;
         next_item<Rows>(a, s, at);
     }
