@@ -329,8 +329,9 @@ def stride_opd_grad(layout: Layout, unit: int, vocab: int, student_logits: torch
 
 class KVCache:
     """Paged cache of keys and values: k and v [n_pages, page_size, n_heads, head_dim] with any strides
-    whose last is 1 (pages may hold heads or tokens in a row), page_table int32 [n_seqs, max_pages].  Holds
-    the caller's tensors; their contents change with every append, the tensors do not."""
+    whose last is 1 (pages may hold heads or tokens in a row), page_table int32 [n_seqs, max_pages] of rows that
+    do not overlap (repeat a row, do not expand it).  Holds the caller's tensors; their contents change with
+    every append, the tensors do not."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
@@ -344,9 +345,11 @@ class KVCache:
         self.k, self.v, self.page_table, self.dtype = k, v, page_table, k.dtype
         self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
         self.n_seqs, self.max_pages = page_table.shape
+        # the stride between rows says nothing where there is one row; rows closer than max_pages are refused by the calls
+        ld = page_table.stride(0) if self.n_seqs > 1 else self.max_pages
         self._c = _CCache(_ptr(k), _ptr(v), _dtype_code(k), self.n_heads, self.head_dim, self.page_size,
-                          self.n_pages, *k.stride()[:3], *v.stride()[:3], _ptr(page_table),
-                          max(page_table.stride(0), self.max_pages), self.n_seqs, self.max_pages)
+                          self.n_pages, *k.stride()[:3], *v.stride()[:3], _ptr(page_table), ld, self.n_seqs,
+                          self.max_pages)
         self.ref = ctypes.byref(self._c)
 
     def c(self):
