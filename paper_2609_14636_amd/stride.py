@@ -458,6 +458,10 @@ def stride_sample(vocab: int, logits: torch.Tensor, noise: torch.Tensor | None,
     if noise is not None and (noise.dtype != torch.float32 or noise.dim() != 2 or noise.shape[0] != n
                               or noise.stride(1) != 1):
         raise ValueError(f"noise must be float32 [{n}, >= vocab] with unit column stride")
+    for name, t in (("logits", logits), ("noise", noise)):
+        # a view of a wider buffer: the call sees its row stride alone
+        if t is not None and t.shape[1] < vocab <= t.stride(0):
+            raise StrideError(1, f"{name} have {t.shape[1]} columns < vocab = {vocab}")
     f32, i32 = torch.float32, torch.int32
     _check(_lib.stride_sample(n, int(vocab), logits.stride(0), _dtype_code(logits), _ptr(logits), _ptr(noise),
                               0 if noise is None else noise.stride(0), _vector("temperature", temperature, n, f32),

@@ -25,3 +25,16 @@ def test_page_table_of_one_row_may_have_any_stride():
     for table in (i32(4).view(1, 4).expand(1, -1), i32(4).as_strided((1, 4), (1, 1)), i32(4).as_strided((1, 4), (0, 1))):
         cache = P.KVCache(torch.zeros(4, 16, 2, 64, dtype=BF), torch.zeros(4, 16, 2, 64, dtype=BF), table)
         assert cache._c.table_ld >= 4
+
+
+@pytest.mark.parametrize("what", ["logits", "noise"])
+def test_sampling_from_views_narrower_than_the_vocabulary(what):
+    """Columns of a wider buffer: its row stride passes the vocabulary, the view's own columns do not, and its last
+    row would be read past its end."""
+    x = dict(logits=torch.zeros(2, 208), noise=torch.zeros(2, 208))
+    x[what] = x[what][:, 104:]
+    buf = torch.zeros(512, dtype=torch.uint8)
+    ws = buf[(-buf.data_ptr()) % 256:][:256]
+    with pytest.raises(P.StrideError) as e:
+        P.stride_sample(150, x["logits"], x["noise"], torch.ones(2), None, None, None, i32(2), None, ws, stream=0)
+    assert e.value.status == 1 and "150" in str(e.value)
