@@ -324,7 +324,7 @@ stride_status stride_records_plan(stride_records *rec, int32_t n_tasks, const in
  *   head_dim      64, 96, 128 or 256
  *   page_size     a power of two up to 65536
  *   page_table    device int32 [n_seqs, max_pages], rows table_ld >= max_pages apart;
- *                 max_pages * page_size is at most 2^31 - 1
+ *                 max_pages * page_size is at most 2^31 - 256
  */
 typedef struct {
     void *k, *v;
@@ -388,7 +388,7 @@ stride_status stride_kv_append(const stride_kv_cache *cache, int64_t n_tokens, c
  *
  *   n_q           rows of q, out [n_q, n_heads_q, head_dim] of the cache's type (strides in elements as in
  *                 stride_kv_append) and lse [n_q, n_heads_q] float, contiguous, or NULL
- *   n_heads_q     a multiple of the cache's n_heads; n_q * n_heads_q is at most 2^31 - 1
+ *   n_heads_q     a multiple of the cache's n_heads; n_q * n_heads_q is at most 2^31 - 256
  *   q_off         [n_seqs + 1] int32, 0 .. n_q, non-decreasing;  ctx_len [n_seqs] int32 >= 0
  *   scale         > 0
  *   ws            at least stride_attention_workspace_size(cache, n_q, n_heads_q) bytes

@@ -92,6 +92,9 @@ stride_status check_domains(const double *table, int32_t n_dom, const char *name
     return STRIDE_OK;
 }
 
+// Keys of a sequence and rows of an attention call are counted in 32 bits, in tiles of up to 256.
+constexpr int32_t kMaxCount = INT32_MAX - 255;
+
 // A stride in elements, or a position in them, that keeps 16-byte accesses aligned.
 bool whole_words(int64_t elements, int32_t dtype) { return elements % (dtype == STRIDE_BF16 ? 8 : 4) == 0; }
 
@@ -107,8 +110,8 @@ stride_status check_cache(const stride_kv_cache *c) {
         return fail(STRIDE_ERR_UNSUPPORTED, "head_dim = %d is not 64, 96, 128 or 256", c->head_dim);
     if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) != 0)
         return fail(STRIDE_ERR_UNSUPPORTED, "page_size = %d is not a power of two in [1, 65536]", c->page_size);
-    if ((int64_t)c->max_pages * c->page_size > INT32_MAX)
-        return fail(STRIDE_ERR_UNSUPPORTED, "max_pages * page_size = %lld passes 2^31 - 1",
+    if ((int64_t)c->max_pages * c->page_size > kMaxCount)
+        return fail(STRIDE_ERR_UNSUPPORTED, "max_pages * page_size = %lld passes 2^31 - 256",
                     (long long)c->max_pages * c->page_size);
     if (c->n_seqs > 0) {
         if (!c->page_table) return fail(STRIDE_ERR_INVALID_ARG, "page_table is NULL");
@@ -519,8 +522,8 @@ stride_status stride_tree_attention(const stride_kv_cache *cache, int64_t n_q, i
     if (n_q < 0) return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld < 0", (long long)n_q);
     if (n_heads_q < 1 || n_heads_q % c.n_heads != 0)
         return fail(STRIDE_ERR_INVALID_ARG, "n_heads_q = %d is not a multiple of n_heads = %d", n_heads_q, c.n_heads);
-    if (n_q > INT32_MAX / n_heads_q)
-        return fail(STRIDE_ERR_UNSUPPORTED, "n_q = %lld rows of %d heads pass 2^31 - 1", (long long)n_q, n_heads_q);
+    if (n_q > kMaxCount / n_heads_q)
+        return fail(STRIDE_ERR_UNSUPPORTED, "n_q = %lld rows of %d heads pass 2^31 - 256", (long long)n_q, n_heads_q);
     if (!(scale > 0.0f && scale < INFINITY)) return fail(STRIDE_ERR_INVALID_ARG, "scale = %g is not > 0", (double)scale);
     if (tree_mask && mask_words < 1) return fail(STRIDE_ERR_INVALID_ARG, "mask_words = %d < 1", mask_words);
     if (n_q > 0 && c.n_seqs == 0) return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld rows but no sequences", (long long)n_q);

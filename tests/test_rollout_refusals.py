@@ -38,3 +38,29 @@ def test_sampling_from_views_narrower_than_the_vocabulary(what):
     with pytest.raises(P.StrideError) as e:
         P.stride_sample(150, x["logits"], x["noise"], torch.ones(2), None, None, None, i32(2), None, ws, stream=0)
     assert e.value.status == 1 and "150" in str(e.value)
+
+
+def aligned(nbytes):
+    buf = torch.zeros(nbytes + 256, dtype=torch.uint8)
+    off = (-buf.data_ptr()) % 256
+    return buf[off:off + nbytes]
+
+
+def test_counts_that_pass_32_bits_within_a_tile():
+    """The last keys of a sequence and the last rows of a call are counted in whole tiles, up to 255 further."""
+    x = torch.zeros(4, 1, 2, 64, dtype=BF)
+    k = torch.zeros(2, 2, 64, dtype=BF)
+    for pages, code in ((2 ** 31 - 1, 2), (2 ** 31 - 255, 2), (2 ** 31 - 256, None)):
+        c = P.KVCache(x, x.clone(), i32(2).view(2, 1))
+        c._c.max_pages = c._c.table_ld = pages
+        # a key that is not 16-byte aligned is refused after the cache has been checked
+        bad = torch.zeros(257, dtype=BF)[1:].view(2, 2, 64)
+        with pytest.raises(P.StrideError) as e:
+            P.stride_kv_append(c, bad, k, i32(2), i32(2), stream=0)
+        assert e.value.status == 2 and ("max_pages" in str(e.value)) == (code is not None), str(e.value)
+    c = P.KVCache(x, x.clone(), i32(2).view(2, 1))
+    for n, heads in ((2 ** 25 - 1, 64), (2 ** 30 - 127, 2)):
+        q = torch.zeros(1, heads, 64, dtype=BF).expand(n, -1, -1)
+        with pytest.raises(P.StrideError) as e:
+            P.stride_tree_attention(c, q, i32(3), i32(2), None, 0.1, q, None, None, aligned(256), stream=0)
+        assert e.value.status == 2 and "2^31 - 256" in str(e.value)
