@@ -94,11 +94,12 @@ stride_status check_domains(const double *table, int32_t n_dom, const char *name
 
 // Keys of a sequence and rows of an attention call are counted in 32 bits, in tiles of up to 256.
 constexpr int32_t kMaxCount = INT32_MAX - 255;
+constexpr int32_t kMaxVocab = 1 << 30;  // that stride_sample takes
 
 // A stride in elements, or a position in them, that keeps 16-byte accesses aligned.
 bool whole_words(int64_t elements, int32_t dtype) { return elements % (dtype == STRIDE_BF16 ? 8 : 4) == 0; }
 
-stride_status check_cache(const stride_kv_cache *c) {
+stride_status check_cache_sizes(const stride_kv_cache *c) {
     if (!c) return fail(STRIDE_ERR_INVALID_ARG, "cache is NULL");
     if (c->dtype != STRIDE_BF16 && c->dtype != STRIDE_F32)
         return fail(STRIDE_ERR_UNSUPPORTED, "dtype %d is neither STRIDE_BF16 nor STRIDE_F32", c->dtype);
@@ -113,6 +114,12 @@ stride_status check_cache(const stride_kv_cache *c) {
     if ((int64_t)c->max_pages * c->page_size > kMaxCount)
         return fail(STRIDE_ERR_UNSUPPORTED, "max_pages * page_size = %lld passes 2^31 - 256",
                     (long long)c->max_pages * c->page_size);
+    return STRIDE_OK;
+}
+
+stride_status check_cache(const stride_kv_cache *c) {
+    const stride_status st = check_cache_sizes(c);
+    if (st != STRIDE_OK) return st;
     if (c->n_seqs > 0) {
         if (!c->page_table) return fail(STRIDE_ERR_INVALID_ARG, "page_table is NULL");
         if (c->table_ld < c->max_pages)
@@ -127,6 +134,19 @@ stride_status check_cache(const stride_kv_cache *c) {
     for (const int64_t x : {c->k_page, c->k_slot, c->k_head, c->v_page, c->v_slot, c->v_head})
         if (!whole_words(x, c->dtype))
             return fail(STRIDE_ERR_UNSUPPORTED, "cache stride %lld is not a multiple of 16 bytes", (long long)x);
+    return STRIDE_OK;
+}
+
+// The sizes of an attention call.
+stride_status check_attention_sizes(const stride_kv_cache &c, int64_t n_q, int32_t n_heads_q) {
+    if (n_q < 0) return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld < 0", (long long)n_q);
+    if (n_heads_q < 1 || n_heads_q % c.n_heads != 0)
+        return fail(STRIDE_ERR_INVALID_ARG, "n_heads_q = %d is not a multiple of n_heads = %d", n_heads_q, c.n_heads);
+    if (n_q > kMaxCount / n_heads_q)
+        return fail(STRIDE_ERR_UNSUPPORTED, "n_q = %lld rows of %d heads pass 2^31 - 256", (long long)n_q, n_heads_q);
+    if (n_q > 0 && c.n_seqs == 0) return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld rows but no sequences", (long long)n_q);
+    if (n_q > 0 && (c.n_pages == 0 || c.max_pages == 0))
+        return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld rows but a cache without pages", (long long)n_q);
     return STRIDE_OK;
 }
 
@@ -505,9 +525,7 @@ stride_status stride_kv_append(const stride_kv_cache *cache, int64_t n_tokens, c
 }
 
 size_t stride_attention_workspace_size(const stride_kv_cache *cache, int64_t n_q, int32_t n_heads_q) {
-    if (!cache || cache->n_heads < 1 || cache->n_seqs < 0 || cache->head_dim < 1 || n_q < 0 || n_heads_q < 1 ||
-        n_heads_q % cache->n_heads != 0)
-        return 0;
+    if (check_cache_sizes(cache) != STRIDE_OK || check_attention_sizes(*cache, n_q, n_heads_q) != STRIDE_OK) return 0;
     return attention_ws_bytes(*cache, n_q, n_heads_q);
 }
 
@@ -519,22 +537,16 @@ stride_status stride_tree_attention(const stride_kv_cache *cache, int64_t n_q, i
     stride_status st = check_cache(cache);
     if (st != STRIDE_OK) return st;
     const stride_kv_cache &c = *cache;
-    if (n_q < 0) return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld < 0", (long long)n_q);
-    if (n_heads_q < 1 || n_heads_q % c.n_heads != 0)
-        return fail(STRIDE_ERR_INVALID_ARG, "n_heads_q = %d is not a multiple of n_heads = %d", n_heads_q, c.n_heads);
-    if (n_q > kMaxCount / n_heads_q)
-        return fail(STRIDE_ERR_UNSUPPORTED, "n_q = %lld rows of %d heads pass 2^31 - 256", (long long)n_q, n_heads_q);
+    st = check_attention_sizes(c, n_q, n_heads_q);
+    if (st != STRIDE_OK) return st;
     if (!(scale > 0.0f && scale < INFINITY)) return fail(STRIDE_ERR_INVALID_ARG, "scale = %g is not > 0", (double)scale);
     if (tree_mask && mask_words < 1) return fail(STRIDE_ERR_INVALID_ARG, "mask_words = %d < 1", mask_words);
-    if (n_q > 0 && c.n_seqs == 0) return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld rows but no sequences", (long long)n_q);
     if (c.n_seqs > 0 && (!q_off || !ctx_len)) return fail(STRIDE_ERR_INVALID_ARG, "q_off or ctx_len is NULL");
     if (n_q > 0) {
         st = check_rows("q", q, q_tok, q_head, c.dtype);
         if (st != STRIDE_OK) return st;
         st = check_rows("out", out, out_tok, out_head, c.dtype);
         if (st != STRIDE_OK) return st;
-        if (c.n_pages == 0 || c.max_pages == 0)
-            return fail(STRIDE_ERR_INVALID_ARG, "n_q = %lld rows but a cache without pages", (long long)n_q);
     }
     st = check_ws(attention_ws_bytes(c, n_q, n_heads_q), ws, ws_bytes);
     if (st != STRIDE_OK) return st;
@@ -546,7 +558,7 @@ stride_status stride_tree_attention(const stride_kv_cache *cache, int64_t n_q, i
 }
 
 size_t stride_sample_workspace_size(int64_t n_rows, int32_t vocab) {
-    if (n_rows < 0 || vocab < 1) return 0;
+    if (n_rows < 0 || vocab < 1 || vocab > kMaxVocab) return 0;
     return sample_ws_bytes(n_rows, vocab);
 }
 
@@ -557,7 +569,7 @@ stride_status stride_sample(int64_t n_rows, int32_t vocab, int64_t ld, int32_t d
                             hipStream_t stream) {
     if (n_rows < 0) return fail(STRIDE_ERR_INVALID_ARG, "n_rows = %lld < 0", (long long)n_rows);
     if (vocab < 1) return fail(STRIDE_ERR_INVALID_ARG, "vocab = %d < 1", vocab);
-    if (vocab > (1 << 30)) return fail(STRIDE_ERR_UNSUPPORTED, "vocab = %d passes 2^30", vocab);
+    if (vocab > kMaxVocab) return fail(STRIDE_ERR_UNSUPPORTED, "vocab = %d passes 2^30", vocab);
     if (ld < vocab) return fail(STRIDE_ERR_INVALID_ARG, "ld = %lld < vocab = %d", (long long)ld, vocab);
     if (dtype != STRIDE_BF16 && dtype != STRIDE_F32)
         return fail(STRIDE_ERR_UNSUPPORTED, "dtype %d is neither STRIDE_BF16 nor STRIDE_F32", dtype);

@@ -64,3 +64,20 @@ def test_counts_that_pass_32_bits_within_a_tile():
         with pytest.raises(P.StrideError) as e:
             P.stride_tree_attention(c, q, i32(3), i32(2), None, 0.1, q, None, None, aligned(256), stream=0)
         assert e.value.status == 2 and "2^31 - 256" in str(e.value)
+
+
+def test_workspace_sizes_of_refused_calls_are_0():
+    x = torch.zeros(4, 16, 2, 64, dtype=BF)
+    c = P.KVCache(x, x.clone(), i32(4).view(2, 2))
+    assert P.stride_attention_workspace_size(c, 3, 4) > 0
+    assert P.stride_attention_workspace_size(c, 2 ** 30, 4) == 0 and P.stride_attention_workspace_size(c, -1, 4) == 0
+    for field, value in (("head_dim", 80), ("page_size", 24), ("dtype", 7), ("max_pages", 2 ** 30), ("n_pages", -1),
+                         ("n_pages", 0), ("n_seqs", 0)):
+        c = P.KVCache(x, x.clone(), i32(4).view(2, 2))
+        setattr(c._c, field, value)
+        assert P.stride_attention_workspace_size(c, 3, 4) == 0, field
+    c = P.KVCache(x, x.clone(), i32(4).view(2, 2))
+    c._c.k = c._c.v = c._c.page_table = None  # only sizes are read
+    assert P.stride_attention_workspace_size(c, 3, 4) > 0
+    assert P.stride_sample_workspace_size(2, 2 ** 30) > 0 and P.stride_sample_workspace_size(2, 2 ** 30 + 1) == 0
+    assert P.stride_sample_workspace_size(-1, 100) == 0
