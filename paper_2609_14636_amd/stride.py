@@ -389,6 +389,8 @@ def stride_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, seq: torc
     q -> q_out) normalised per head with their weights and rotated to pos on the way."""
     n = k.shape[0]
     heads, q_args, qo_args = 0, (None, 0, 0), (None, 0, 0)
+    if q is None and q_out is not None:
+        raise ValueError("q_out given without q")
     if q is not None:
         if q_out is None:
             raise ValueError("q given without q_out")

@@ -81,3 +81,9 @@ def test_workspace_sizes_of_refused_calls_are_0():
     assert P.stride_attention_workspace_size(c, 3, 4) > 0
     assert P.stride_sample_workspace_size(2, 2 ** 30) > 0 and P.stride_sample_workspace_size(2, 2 ** 30 + 1) == 0
     assert P.stride_sample_workspace_size(-1, 100) == 0
+
+
+def test_query_outputs_without_queries():
+    x, k = torch.zeros(4, 16, 2, 64, dtype=BF), torch.zeros(2, 2, 64, dtype=BF)
+    with pytest.raises(ValueError):
+        P.stride_kv_append(P.KVCache(x, x.clone(), i32(4).view(2, 2)), k, k, i32(2), i32(2), q_out=k.clone(), stream=0)
