@@ -147,6 +147,23 @@ __device__ __forceinline__ uint64_t block_max(uint64_t x, Shared &sh) {
     for (int i = 1; i < kWaves; ++i) x = sh.wave64[i] > x ? sh.wave64[i] : x;
     return x;
 }
+// The same with a float's maximum beside it.
+__device__ __forceinline__ uint64_t block_max(uint64_t x, float &y, Shared &sh) {
+    x = wave_max(x);
+    y = wave_max(y);
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) {
+        sh.wave64[threadIdx.x / kWave] = x;
+        sh.wavef[threadIdx.x / kWave].x = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        x = sh.wave64[i] > x ? sh.wave64[i] : x;
+        y = fmaxf(y, sh.wavef[i].x);
+    }
+    return x;
+}
 // The largest of two values at once.
 __device__ __forceinline__ float2 block_max2(float x, float y, Shared &sh) {
     float2 r = make_float2(wave_max(x), wave_max(y));
@@ -327,6 +344,35 @@ __device__ __attribute__((noinline)) Found first_entry(const Row<DT> row, Shared
 
 // s - log noise of one entry, in units of log 2 (s2 = s log2 e).
 __device__ __forceinline__ float race(float s2, float noise) { return s2 - lg2(noise); }
+
+// Keys of unfiltered rows are relative to the largest of the first entries, which the pass does not have to look for: near
+// the row's largest, so that a key's rounding is that of a small number.  Where it is not (the first entries masked by
+// large values, a small T), keys come out of it with fewer bits than the noise needs, and a second pass takes them
+// relative to the largest entry.  Up to kFar, in units of log 2, the rounding is 2^-24 kFar = 4e-6 at most.
+constexpr float kFar = 64.0f;
+__device__ __forceinline__ bool too_far(float top, float ref, float c) { return top > -INFINITY && !(fabsf(top - ref) * c <= kFar); }
+
+// The largest key, relative to `ref`, of this thread's words among [begin, end), with its index (0: none).
+template <int DT, int Threads>
+__device__ __attribute__((noinline)) uint64_t race_again(const Row<DT> row, const float *noise, float c, float ref, int begin, int end) {
+    constexpr int E = Elem<DT>::n;
+    float top = -INFINITY;
+    int at = -1;
+    for (int i = begin + (int)threadIdx.x; i < end; i += Threads) {
+        float x[E];
+        widen<DT>(row.masked(row.load(i), i), x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (!(x[e] > -INFINITY)) continue;
+            const float key = __builtin_fmaf(x[e] - ref, c, -lg2(noise[i * E + e]));
+            if (key > top) {
+                top = key;
+                at = i * E + e;
+            }
+        }
+    }
+    return at < 0 ? (uint64_t)0 : entry(top, at);
+}
 
 struct Filter {
     float c, min_s2;     // log2 e / T; the least s that min-p keeps, in units of log 2
@@ -654,9 +700,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
         float top = -INFINITY, ref = 0.0f;
         int at = -1;
         if (temp > 0.0f) {
-            // the point that keys are relative to: the largest of the part's first entries, or for a small T of all
-            if (temp < 0x1p-10f) each([&](const u32x4 &w, int) __attribute__((always_inline)) { largest.add(w); });
-            else largest.add(held[0]);
+            // the point that keys are relative to: the largest of the part's first entries
+            largest.add(held[0]);
             const float m = wave_max(largest.bad() ? -INFINITY : largest.value());
             if (lane == 0) s_ends[wave].x = m;
             __syncthreads();
@@ -686,13 +731,31 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
             }
         });
         const uint64_t m = wave_max(at < 0 ? (uint64_t)0 : entry(top, at));
-        if (lane == 0) s_best[wave] = m;
+        const float wm = wave_max(largest.value());
+        if (lane == 0) {
+            s_best[wave] = m;
+            s_ends[wave].y = wm;
+        }
         if (largest.bad()) s_bad = 1;
         __syncthreads();
-        if (tid == 0) {
-            uint64_t best = s_best[0];
+        uint64_t best = s_best[0];
+        float most = s_ends[0].y;
+#pragma unroll
+        for (int i = 1; i < kPartWaves; ++i) {
+            best = s_best[i] > best ? s_best[i] : best;
+            most = fmaxf(most, s_ends[i].y);
+        }
+        if (temp > 0.0f && !s_bad && too_far(most, ref, f.c)) {  // the same for the whole workgroup
+            ref = most;
+            const uint64_t again = wave_max(race_again<DT, kPartThreads>(row, noise, f.c, ref, begin, end));
+            __syncthreads();
+            if (lane == 0) s_best[wave] = again;
+            __syncthreads();
+            best = s_best[0];
 #pragma unroll
             for (int i = 1; i < kPartWaves; ++i) best = s_best[i] > best ? s_best[i] : best;
+        }
+        if (tid == 0) {
             out.first = best;
             out.at = best ? (int32_t)~(uint32_t)best : -1;
             out.ref = ref;
@@ -800,7 +863,8 @@ __device__ __forceinline__ Found from_parts(const SampleArgs &a, int64_t r, cons
         if (at >= 0) {
             const float z = DT == STRIDE_BF16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(row.p)[at] << 16)
                                               : reinterpret_cast<const float *>(row.p)[at];
-            x = entry(__builtin_fmaf(z - ref, f.c, -lg2(noise[at])), at);
+            const float key = __builtin_fmaf(z - ref, f.c, -lg2(noise[at]));
+            if (key > -INFINITY) x = entry(key, at);
         }
         const uint64_t best = wave_max(x);
         return {best, best != 0};  // no noise that can win: the first entry, which the parts do not have
@@ -899,18 +963,10 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         best = x.best;
         bad = x.yes;
     } else if (plain) {
-        // keys relative to the largest of the row's first entries: near the row's largest, so that a key's
-        // rounding is that of a small number; for small T, where that would not do, to the row's largest
-        float ref;
-        if (temp < 0x1p-10f) {
-            const uint64_t top = first_entry<DT>(row, sh).best;
-            ref = top ? value_of((uint32_t)(top >> 32)) : 0.0f;
-        } else {
-            Largest<DT> first;
-            first.add(row.masked(row.load(tid), tid));
-            ref = block_max2(first.bad() ? -INFINITY : first.value(), 0.0f, sh).x;
-            if (!(fabsf(ref) < INFINITY)) ref = 0.0f;
-        }
+        Largest<DT> first;
+        first.add(row.masked(row.load(tid), tid));
+        float ref = block_max2(first.bad() ? -INFINITY : first.value(), 0.0f, sh).x;
+        if (!(fabsf(ref) < INFINITY)) ref = 0.0f;
         float top = -INFINITY;
         int at = -1;
         const u32x4 *nw = reinterpret_cast<const u32x4 *>(noise);
@@ -948,7 +1004,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
             }
         }
         bad |= seen.bad();
-        best = block_max(at < 0 ? (uint64_t)0 : entry(top, at), sh);
+        float most = seen.bad() ? -INFINITY : seen.value();
+        best = block_max(at < 0 ? (uint64_t)0 : entry(top, at), most, sh);
+        if (too_far(most, ref, f.c)) best = block_max(race_again<DT, kThreads>(row, noise, f.c, most, 0, words), sh);
     } else {
         // ---- first pass: every thread's maximum ----
         Largest<DT> largest;
