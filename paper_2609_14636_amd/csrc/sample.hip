@@ -376,12 +376,12 @@ __device__ __attribute__((noinline)) uint64_t race_again(const Row<DT> row, cons
 
 struct Filter {
     float c, min_s2;     // log2 e / T; the least s that min-p keeps, in units of log 2
-    float top, top_c, top_p;  // the row's largest z, and times c
+    float top, top_p;    // top: the row's largest z
     int k;               // 0: all
     bool p;
 };
-// s in units of log 2: one rounding near the top, and the same one of top * c for every entry.
-__device__ __forceinline__ float s2_of(const Filter &f, float x) { return __builtin_fmaf(x, f.c, -f.top_c); }
+// s in units of log 2: 0 for the largest z, whatever its size and the temperature.
+__device__ __forceinline__ float s2_of(const Filter &f, float x) { return (x - f.top) * f.c; }
 // Mass of an entry in units of 2^-40 of the largest one's.
 __device__ __forceinline__ uint64_t mass_of(const Filter &f, float x) { return (uint64_t)(ex2(s2_of(f, x)) * kMassUnit); }
 
@@ -777,7 +777,6 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
     }
     low = -low;
     f.top = top;
-    f.top_c = top * f.c;
     const bool row_mass = f.p && !f.k;
     const float scale = low < top ? (float)(kCutBins - 1) / (top - low) : 0.0f;
     const bool sharp = scale > 0.0f && scale < INFINITY;
@@ -871,8 +870,7 @@ __device__ __forceinline__ Found from_parts(const SampleArgs &a, int64_t r, cons
     }
     f.top = wave_max(mine ? head.top : -INFINITY);
     if (!(f.top > -INFINITY)) return {0, true};
-    f.top_c = f.top * f.c;
-    if (!(fabsf(f.top_c) < INFINITY) || __any(mine && head.n > kPartList)) return {0, false};
+    if (__any(mine && head.n > kPartList)) return {0, false};
     const float cut = wave_max(mine ? head.cut : -INFINITY);  // all entries from here on are in the lists
     double whole = 0.0;
     if (f.p && !f.k) {
@@ -1016,15 +1014,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         if (bad) sh.bad = 1;
         const float2 ends = block_max2(mine, mine > -INFINITY ? -mine : -INFINITY, sh);
         f.top = ends.x;
-        f.top_c = f.top * f.c;
         const float low = -ends.y;
-        bool wrong = sh.bad || !(f.top > -INFINITY);
-        // a product that overflows (a temperature near 0 beside large logits): the first entry is all there is
-        if (!(fabsf(f.top_c) < INFINITY)) {
-            if (!wrong) best = first_entry<DT>(row, sh).best;
-            wrong = true;
-        }
-        if (!wrong) {
+        if (!sh.bad && f.top > -INFINITY) {
             // ---- the cut, the entries above it, and the row's mass for top-p alone ----
             const float scale = low < f.top ? (float)(kCutBins - 1) / (f.top - low) : 0.0f;
             const bool row_mass = f.p && !f.k, sharp = scale > 0.0f && scale < INFINITY;

@@ -74,3 +74,47 @@ def test_unfiltered_rows_of_large_values(dtype, rows):
         z = z.to(dtype)
         for temp in (1.0, 5.0, 1e-3, 1e-12):
             check(z, vocab, noise, temp, call(z.cuda(), vocab, noise.cuda(), temp))
+
+
+def tied(rows, vocab, dtype, ties, seed):
+    """Rows whose largest value, near 18, is at `ties` places; the others are half a unit lower and more."""
+    z, noise, g = buffers(rows, vocab, dtype, seed)
+    at = torch.stack([torch.randperm(vocab, generator=g)[:ties].sort().values for _ in range(rows)])
+    top = (17.0 + 2.0 * torch.rand(rows, 1, generator=g)).to(dtype)
+    z = torch.minimum(z, top - 0.5)
+    z.scatter_(1, at, top.expand(-1, ties).contiguous())
+    return z, noise, at
+
+
+def smallest(noise, at, kept):
+    return [int(at[r, noise[r, at[r, :kept]].argmin()]) for r in range(len(at))]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,vocab", [(5, 900), (5, 40000), (140, 40000)])
+@pytest.mark.parametrize("ties", [2, 6, 600, 3000])
+def test_tied_largest_values(dtype, rows, vocab, ties):
+    """exp(s) is 1 for them: min-p of 1 keeps all, top-p by their number, and the smallest random number wins."""
+    ties = min(ties, vocab // 2)
+    z, noise, at = tied(rows, vocab, dtype, ties, seed=ties)
+    zc, nc = z.cuda(), noise.cuda()
+    for temp, k, p, low, kept in ((1.0, 0, 1.0, 1.0, ties), (1.0, 0, 1.0, 0.9, ties), (0.7, 0, 1.0, 1.0, ties),
+                                  (1.0, 4000, 1.0, 1.0, ties), (1e-4, 0, 1.0, 0.0, ties), (1e-4, 0, 1.0, 0.9, ties),
+                                  (1e-6, 0, 1.0, 1.0, ties), (1e-6, 40, 1.0, 0.0, min(40, ties)), (1e-6, 0, 0.5, 0.0, ties // 2),
+                                  (1e-8, 0, 0.5, 0.9, ties // 2), (1e-8, 2, 1.0, 0.0, 2), (1e-8, 0, 1.0, 0.0, ties),
+                                  (1e-20, 0, 0.5, 0.0, ties // 2), (1e-20, 0, 1.0, 0.5, ties), (1e-35, 0, 0.5, 0.0, ties // 2),
+                                  (1e-35, 10 ** 6, 1.0, 0.1, ties), (1e-35, 2000, 0.5, 0.0, min(1000, ties // 2))):
+        got = call(zc, vocab, nc, temp, k, p, low)
+        assert got == smallest(noise, at, kept), (temp, k, p, low)
+
+
+@pytest.mark.parametrize("rows,vocab", [(5, 900), (5, 40000), (140, 40000)])
+def test_the_largest_temperature(rows, vocab):
+    """All finite logits are one then: the smallest random number wins among those that are kept."""
+    z, noise, g = buffers(rows, vocab, F32, seed=23)
+    z[:, :vocab][torch.rand(rows, vocab, generator=g) < 0.5] = -torch.inf
+    inside = z[:, :vocab].clone()
+    for k in (0, 10):
+        kept = inside > -torch.inf if k == 0 else inside >= inside.topk(k, 1).values[:, -1:]
+        want = torch.where(kept, noise[:, :vocab], torch.inf).argmin(1).tolist()
+        assert call(z.cuda(), vocab, noise.cuda(), 3e38, k) == want
