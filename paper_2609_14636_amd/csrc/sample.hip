@@ -87,7 +87,8 @@ struct Shared {
 };
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }
+__device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }  // takes subnormal x for 0
+__device__ __forceinline__ float lg2_all(float x) { return x < 0x1p-126f ? lg2(x * 0x1p32f) - 32.0f : lg2(x); }
 
 // Bits of x in the order of its values; -0 and 0 are one value.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -343,14 +344,16 @@ __device__ __attribute__((noinline)) Found first_entry(const Row<DT> row, Shared
 }
 
 // s - log noise of one entry, in units of log 2 (s2 = s log2 e).
-__device__ __forceinline__ float race(float s2, float noise) { return s2 - lg2(noise); }
+__device__ __forceinline__ float race(float s2, float noise) { return s2 - lg2_all(noise); }
 
 // Keys of unfiltered rows are relative to the largest of the first entries, which the pass does not have to look for: near
 // the row's largest, so that a key's rounding is that of a small number.  Where it is not (the first entries masked by
 // large values, a small T), keys come out of it with fewer bits than the noise needs, and a second pass takes them
-// relative to the largest entry.  Up to kFar, in units of log 2, the rounding is 2^-24 kFar = 4e-6 at most.
+// relative to the largest entry; also where the winner's noise may be subnormal.  Up to kFar, in units of log 2, the rounding is 2^-24 kFar = 4e-6 at most.
 constexpr float kFar = 64.0f;
-__device__ __forceinline__ bool too_far(float top, float ref, float c) { return top > -INFINITY && !(fabsf(top - ref) * c <= kFar); }
+__device__ __forceinline__ bool not_settled(uint64_t best, float top, float ref, float c) {
+    return top > -INFINITY && (!(fabsf(top - ref) * c <= kFar) || (uint32_t)(best >> 32) == ordered(INFINITY));
+}
 
 // The largest key, relative to `ref`, of this thread's words among [begin, end), with its index (0: none).
 template <int DT, int Threads>
@@ -364,7 +367,7 @@ __device__ __attribute__((noinline)) uint64_t race_again(const Row<DT> row, cons
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if (!(x[e] > -INFINITY)) continue;
-            const float key = __builtin_fmaf(x[e] - ref, c, -lg2(noise[i * E + e]));
+            const float key = __builtin_fmaf(x[e] - ref, c, -lg2_all(noise[i * E + e]));
             if (key > top) {
                 top = key;
                 at = i * E + e;
@@ -632,7 +635,7 @@ __device__ __forceinline__ bool parameters(const SampleArgs &a, int64_t r, float
     f.k = top_k > 0 && top_k < a.vocab ? top_k : 0;
     f.p = top_p < 1.0f;
     f.top_p = top_p;
-    f.min_s2 = min_p > 0.0f ? lg2(min_p) : -INFINITY;
+    f.min_s2 = min_p > 0.0f ? lg2_all(min_p) : -INFINITY;
     plain = f.k == 0 && !f.p && min_p == 0.0f;
     return temp >= 0.0f && temp < INFINITY && top_p == top_p && min_p >= 0.0f;
 }
@@ -745,7 +748,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
             best = s_best[i] > best ? s_best[i] : best;
             most = fmaxf(most, s_ends[i].y);
         }
-        if (temp > 0.0f && !s_bad && too_far(most, ref, f.c)) {  // the same for the whole workgroup
+        if (temp > 0.0f && !s_bad && not_settled(best, most, ref, f.c)) {  // the same for the whole workgroup
             ref = most;
             const uint64_t again = wave_max(race_again<DT, kPartThreads>(row, noise, f.c, ref, begin, end));
             __syncthreads();
@@ -862,7 +865,7 @@ __device__ __forceinline__ Found from_parts(const SampleArgs &a, int64_t r, cons
         if (at >= 0) {
             const float z = DT == STRIDE_BF16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(row.p)[at] << 16)
                                               : reinterpret_cast<const float *>(row.p)[at];
-            const float key = __builtin_fmaf(z - ref, f.c, -lg2(noise[at]));
+            const float key = __builtin_fmaf(z - ref, f.c, -lg2_all(noise[at]));
             if (key > -INFINITY) x = entry(key, at);
         }
         const uint64_t best = wave_max(x);
@@ -1004,7 +1007,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         bad |= seen.bad();
         float most = seen.bad() ? -INFINITY : seen.value();
         best = block_max(at < 0 ? (uint64_t)0 : entry(top, at), most, sh);
-        if (too_far(most, ref, f.c)) best = block_max(race_again<DT, kThreads>(row, noise, f.c, most, 0, words), sh);
+        if (not_settled(best, most, ref, f.c)) best = block_max(race_again<DT, kThreads>(row, noise, f.c, most, 0, words), sh);
     } else {
         // ---- first pass: every thread's maximum ----
         Largest<DT> largest;

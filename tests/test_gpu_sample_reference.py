@@ -118,3 +118,21 @@ def test_the_largest_temperature(rows, vocab):
         kept = inside > -torch.inf if k == 0 else inside >= inside.topk(k, 1).values[:, -1:]
         want = torch.where(kept, noise[:, :vocab], torch.inf).argmin(1).tolist()
         assert call(z.cuda(), vocab, noise.cuda(), 3e38, k) == want
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,vocab", [(4, 900), (4, 40000), (140, 20000)])
+@pytest.mark.parametrize("k,p,low", [(0, 1.0, 0.0), (50, 1.0, 0.0), (0, 1 - 2.0 ** -24, 0.0), (0, 1.0, 1e-35), (4000, 1.0, 0.0)])
+def test_random_numbers_below_the_normal_range(dtype, rows, vocab, k, p, low):
+    """2^-133 and 2^-131 are random numbers like others: their logarithms count, and 0 alone always wins."""
+    z, noise, _ = buffers(rows, vocab, dtype, seed=5)
+    z[:, [100, 300, 700]] = torch.tensor([30.0, 30.0, 40.0], dtype=dtype)
+    noise[:, 100], noise[:, 300], noise[:, 700] = 2.0 ** -131, 2.0 ** -133, 1.0
+    # keys: -10 + 90.8, -10 + 92.2, 0
+    assert call(z.cuda(), vocab, noise.cuda(), 1.0, k, p, low) == [300] * rows
+    z[:, 700] = 130.0  # -100 + 90.8, -100 + 92.2, 0
+    assert call(z.cuda(), vocab, noise.cuda(), 1.0, k, p, low) == [700] * rows
+    z[:, 700] = 40.0
+    noise[:, 310] = 0.0
+    z[:, 310] = 30.0
+    assert call(z.cuda(), vocab, noise.cuda(), 1.0, k, p, low) == [310] * rows
