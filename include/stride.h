@@ -397,7 +397,8 @@ stride_status stride_kv_append(const stride_kv_cache *cache, int64_t n_tokens, c
  * weights are rounded to bf16 for the product with v (in float nothing is rounded below 32 bits).
  * Data errors: offsets that decrease or leave [0, n_q] raise STRIDE_FLAG_BAD_OFFSETS and the rows of no
  * sequence are not written; a negative ctx_len, or one whose new tokens pass max_pages * page_size, raises
- * STRIDE_FLAG_BAD_OFFSETS, and a page id outside [0, n_pages) STRIDE_FLAG_BAD_PAGE: rows that read it are NaN.
+ * STRIDE_FLAG_BAD_OFFSETS and the sequence's rows are NaN; a page id outside [0, n_pages) of a sequence's tokens
+ * raises STRIDE_FLAG_BAD_PAGE, and the rows that see a key of that page are NaN.
  */
 stride_status stride_tree_attention(const stride_kv_cache *cache, int64_t n_q, int32_t n_heads_q,
                                     const void *q, int64_t q_tok, int64_t q_head, const int32_t *q_off,

@@ -135,7 +135,7 @@ __device__ __forceinline__ void wait_vmem() {
 
 struct Seq {
     int off, n, ctx;
-    bool bad;  // lengths that the page table cannot hold: its rows are NaN
+    bool bad;  // lengths that the page table cannot hold: all its rows are NaN
 };
 
 __device__ __forceinline__ Seq sequence(const AttendArgs &a, int s, uint32_t &flag) {
@@ -352,12 +352,17 @@ __device__ __forceinline__ int32_t scalar_load(const int32_t *p) {
     return *(const __attribute__((address_space(4))) int32_t *)p;
 }
 
-// The page id, or the first page in the place of one outside the cache.
-__device__ __forceinline__ int32_t checked_page(const AttendArgs &a, int32_t page, bool &poison) {
-    const bool ok = page >= 0 && page < a.n_pages;
-    poison |= !ok;
+// The page id, or the first page in the place of one outside the cache.  The rows that see its keys are NaN and no others:
+// all rows where a block is whole, else the keys are made NaN.  `lost`: whether any of the wave's was outside; which is
+// looked up again where there is one.
+__device__ __forceinline__ bool in_cache(const AttendArgs &a, int32_t page) { return page >= 0 && page < a.n_pages; }
+template <bool Uniform>
+__device__ __forceinline__ int32_t checked_page(const AttendArgs &a, int32_t page, bool &lost) {
+    const bool ok = in_cache(a, page);
+    lost |= Uniform ? !ok : __any(!ok) != 0;
     return ok ? page : 0;
 }
+__device__ __forceinline__ u32x4 nan_word() { return u32x4{~0u, ~0u, ~0u, ~0u}; }  // of bf16 or float
 
 // Non-finite elements of a word become zeros; whether there were any.
 template <int DT>
@@ -426,7 +431,7 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
         const int32_t *table = a.table + at.seq * a.table_ld;
         const char *kb = static_cast<const char *>(a.k) + at.head * a.k_head * Ty::size;
         const char *vb = static_cast<const char *>(a.v) + at.head * a.v_head * Ty::size;
-        bool poison = s.bad;
+        bool lost = false, any_lost = false, poison = s.bad;  // pages outside the cache: of the block on its way, of all
 
         Wave<DT, D, RT> x;
 #pragma unroll
@@ -474,8 +479,9 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
             }
         };
         auto fetch = [&](int blk, B &x) __attribute__((always_inline)) {
+            lost = false;
             if (OnePage) {  // slots past the sequence's end are the page's own
-                const int32_t page = checked_page(a, pg[0], poison);
+                const int32_t page = checked_page<true>(a, pg[0], lost);
                 const int64_t slot = (blk * KB) & ((1 << a.page_shift) - 1);
                 const char *kp = kb + (page * a.k_page + slot * a.k_slot) * Ty::size;
                 const char *vp = vb + (page * a.v_page + slot * a.v_slot) * Ty::size;
@@ -488,7 +494,7 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
                 for (int i = 0; i < B::N; ++i) {
                     int key = blk * KB + row_of(i);
                     key = key < len ? key : len - 1;
-                    const int32_t page = checked_page(a, pg[i], poison);
+                    const int32_t page = checked_page<false>(a, pg[i], lost);
                     const int64_t slot = key & ((1 << a.page_shift) - 1);
                     x.k[i] = once(kb + (page * a.k_page + slot * a.k_slot) * Ty::size + word_of(i) * 16);
                     x.v[i] = once(vb + (page * a.v_page + slot * a.v_slot) * Ty::size + word_of(i) * 16);
@@ -505,12 +511,16 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
             const int k0 = b * KB;
             const bool tail = k0 + KB > s.ctx;  // the same for the whole wave: some keys are not every row's
             bool dirty = false;
+            any_lost |= lost;
+            poison |= lost && !tail;
             if (tail) {
 #pragma unroll
                 for (int i = 0; i < B::N; ++i) {
                     const int key = k0 + row_of(i);
                     if (key >= len) next.v[i] = u32x4{};
                     else if (key >= s.ctx) dirty |= scrub<DT>(next.v[i]);
+                    if (lost && (OnePage || !in_cache(a, table[(key < len ? key : len - 1) >> a.page_shift])))
+                        next.k[i] = nan_word();
                 }
             }
 #pragma unroll
@@ -642,8 +652,8 @@ __global__ __launch_bounds__(kThreads, Occ) void attend_kernel(AttendArgs a) {
         }
 
         // ---- join the waves, one row tile after the other ----
-        if (__any(poison)) {
-            raise_flag(a.flags, s.bad ? 0u : (uint32_t)STRIDE_FLAG_BAD_PAGE);
+        if (any_lost) raise_flag(a.flags, STRIDE_FLAG_BAD_PAGE);
+        if (poison) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) x.l[t] = __builtin_nanf("");
         }
@@ -818,7 +828,7 @@ __device__ __forceinline__ void attend_wide(const AttendArgs &a) {
         const bool busy = r0 < n_rows;                          // the wave has rows
         const bool in = r < n_rows;
         const int tok = in ? r / a.group : 0;
-        bool poison = s.bad;
+        bool lost = false, any_lost = false, poison = s.bad;  // pages outside the cache: of the tile on its way, of all
         // keys that all rows of the workgroup see, and one past the last that a row of this wave sees
         int all_see = s.ctx, wave_end = len;
         if (!a.mask) {
@@ -861,8 +871,9 @@ __device__ __forceinline__ void attend_wide(const AttendArgs &a) {
         auto load = [&](int t, char *buf, auto aux) __attribute__((always_inline)) {
             constexpr int Aux = decltype(aux)::value;
             char *dst = buf + wave * 1024;
+            lost = false;
             if (OnePage) {  // slots past the sequence's end are the page's own
-                const int32_t page = checked_page(a, pg[0], poison);
+                const int32_t page = checked_page<true>(a, pg[0], lost);
                 const int64_t slot = (t * kTile) & ((1 << a.page_shift) - 1);
                 const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
                     (void *)(kb + page * a.k_page + slot * a.k_slot), (short)0, (int)((63 * a.k_slot + D) * 2), kBufferFlags);
@@ -878,7 +889,7 @@ __device__ __forceinline__ void attend_wide(const AttendArgs &a) {
                 for (int i = 0; i < W::N; ++i) {
                     int key = t * kTile + word(i) / W::words;
                     key = key < len ? key : len - 1;
-                    const int32_t page = checked_page(a, pg[i], poison);
+                    const int32_t page = checked_page<false>(a, pg[i], lost);
                     const int64_t slot = key & ((1 << a.page_shift) - 1);
                     const char *kp = reinterpret_cast<const char *>(kb + page * a.k_page + slot * a.k_slot) + koff[i];
                     const char *vp = reinterpret_cast<const char *>(vb + page * a.v_page + slot * a.v_slot) + voff[i];
@@ -921,6 +932,16 @@ __device__ __forceinline__ void attend_wide(const AttendArgs &a) {
         auto step = [&](char *base, char *other, auto tail_tag) __attribute__((always_inline)) {
             constexpr bool Tail = decltype(tail_tag)::value;
             wait_vmem<0>();  // this thread's part of tile t
+            any_lost |= lost;
+            if (OnePage && !Tail) {  // the same page for all waves
+                poison |= lost;
+            } else if (lost) {
+                for (int i = 0; i < W::N; ++i) {
+                    const int key = t * kTile + word(i) / W::words;
+                    if (OnePage || !in_cache(a, table[(key < len ? key : len - 1) >> a.page_shift]))
+                        *reinterpret_cast<u32x4 *>(base + word(i) * 16) = nan_word();
+                }
+            }
             if (Tail) clean(t, base);
             __syncthreads();  // all of it, and tile t - 1 has been read
             if (t + 1 < stop) {
@@ -1037,18 +1058,8 @@ __device__ __forceinline__ void attend_wide(const AttendArgs &a) {
         for (int odd = 0; t < stop; ++t, odd ^= 1) step(odd ? lds1 : lds0, odd ? lds0 : lds1, std::true_type());
 
         // ---- results: a lane has 4 consecutive elements of its row at a time ----
-        bool nan = s.bad;
-        if (OnePage) {
-            nan = poison;  // the same for the whole workgroup
-        } else {
-            const bool lost = __any(poison);
-            __syncthreads();  // every wave is past the last tile
-            if (lane == 0) s_dirty[0][wave] = lost;
-            __syncthreads();
-            nan = (s_dirty[0][0] | s_dirty[0][1] | s_dirty[0][2] | s_dirty[0][3]) != 0;
-        }
-        if (nan && !s.bad) raise_flag(a.flags, STRIDE_FLAG_BAD_PAGE);
-        l = nan ? __builtin_nanf("") : half_sum(l);
+        if (any_lost) raise_flag(a.flags, STRIDE_FLAG_BAD_PAGE);
+        l = poison ? __builtin_nanf("") : half_sum(l);
         const bool whole = at.unit == 0 && u1 == units;
         if (in) {
             const int head = at.head * a.group + r - tok * a.group, row = wave * 32 + col;
