@@ -525,65 +525,65 @@ __device__ __attribute__((noinline)) Found choose(uint32_t n, bool whole_list, d
     const int tid = threadIdx.x;
     const bool row_mass = f.p && !f.k;
     uint64_t *list = sh.mass;
-                    // ---- of each entry: its rank, the mass before it and its own ----
-                    const int per = n <= kCount ? 1 : 2;
-                    uint64_t x[2] = {0, 0}, m[2] = {0, 0}, before[2] = {0, 0}, all = 0;
-                    uint32_t rank[2] = {0, 0};
-                    if (per == 1) {
-                        constexpr uint32_t kStep = 8;  // entries asked for at once
-                        if (tid < (int)n) {
-                            x[0] = list[tid];
-                            m[0] = mass_of(f, value_of((uint32_t)(x[0] >> 32)));
-                        }
-                        if (tid < (int)(n + kStep - 1)) {
-                            sh.pair[tid][0] = x[0];
-                            sh.pair[tid][1] = m[0];
-                        }
-                        __syncthreads();
-                        if ((tid & ~(kWave - 1)) < (int)n) {  // the waves that have entries
-                            for (uint32_t i = 0; i < n; i += kStep) {
-                                ulonglong2 y[kStep];
-    #pragma unroll
-                                for (uint32_t j = 0; j < kStep; ++j) y[j] = *reinterpret_cast<const ulonglong2 *>(sh.pair[i + j]);
-    #pragma unroll
-                                for (uint32_t j = 0; j < kStep; ++j) {
-                                    const bool more = y[j].x > x[0];
-                                    rank[0] += more;
-                                    before[0] += more ? y[j].y : 0;
-                                }
-                            }
-                            const uint32_t last = (f.k && (uint32_t)f.k < n ? (uint32_t)f.k : n) - 1;
-                            if (tid < (int)n && rank[0] == last) sh.above_mass = before[0] + m[0];
-                        }
-                        __syncthreads();
-                        all = sh.above_mass;
-                    } else {  // sorted, largest first (a bitonic network)
-                        uint32_t size = 2;
-                        while (size < n) size *= 2;
-                        for (uint32_t i = n + tid; i < size; i += kThreads) list[i] = 0;
-                        for (uint32_t span = 2; span <= size; span *= 2)
-                            for (uint32_t step = span / 2; step > 0; step /= 2) {
-                                __syncthreads();
-                                for (uint32_t t = tid; t < size / 2; t += kThreads) {
-                                    const uint32_t i = 2 * t - (t & (step - 1)), j = i + step;
-                                    const uint64_t u = list[i], v = list[j];
-                                    if ((u < v) == ((i & span) == 0)) {
-                                        list[i] = v;
-                                        list[j] = u;
-                                    }
-                                }
-                            }
-                        __syncthreads();
-    #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            rank[j] = 2 * tid + j;
-                            x[j] = rank[j] < n ? list[rank[j]] : 0;
-                            if (rank[j] < n && (f.k == 0 || rank[j] < (uint32_t)f.k))
-                                m[j] = mass_of(f, value_of((uint32_t)(x[j] >> 32)));
-                        }
-                        before[0] = block_before(m[0] + m[1], all, sh);
-                        before[1] = before[0] + m[0];
+    // ---- of each entry: its rank, the mass before it and its own ----
+    const int per = n <= kCount ? 1 : 2;
+    uint64_t x[2] = {0, 0}, m[2] = {0, 0}, before[2] = {0, 0}, all = 0;
+    uint32_t rank[2] = {0, 0};
+    if (per == 1) {
+        constexpr uint32_t kStep = 8;  // entries asked for at once
+        if (tid < (int)n) {
+            x[0] = list[tid];
+            m[0] = mass_of(f, value_of((uint32_t)(x[0] >> 32)));
+        }
+        if (tid < (int)(n + kStep - 1)) {
+            sh.pair[tid][0] = x[0];
+            sh.pair[tid][1] = m[0];
+        }
+        __syncthreads();
+        if ((tid & ~(kWave - 1)) < (int)n) {  // the waves that have entries
+            for (uint32_t i = 0; i < n; i += kStep) {
+                ulonglong2 y[kStep];
+#pragma unroll
+                for (uint32_t j = 0; j < kStep; ++j) y[j] = *reinterpret_cast<const ulonglong2 *>(sh.pair[i + j]);
+#pragma unroll
+                for (uint32_t j = 0; j < kStep; ++j) {
+                    const bool more = y[j].x > x[0];
+                    rank[0] += more;
+                    before[0] += more ? y[j].y : 0;
+                }
+            }
+            const uint32_t last = (f.k && (uint32_t)f.k < n ? (uint32_t)f.k : n) - 1;
+            if (tid < (int)n && rank[0] == last) sh.above_mass = before[0] + m[0];
+        }
+        __syncthreads();
+        all = sh.above_mass;
+    } else {  // sorted, largest first (a bitonic network)
+        uint32_t size = 2;
+        while (size < n) size *= 2;
+        for (uint32_t i = n + tid; i < size; i += kThreads) list[i] = 0;
+        for (uint32_t span = 2; span <= size; span *= 2)
+            for (uint32_t step = span / 2; step > 0; step /= 2) {
+                __syncthreads();
+                for (uint32_t t = tid; t < size / 2; t += kThreads) {
+                    const uint32_t i = 2 * t - (t & (step - 1)), j = i + step;
+                    const uint64_t u = list[i], v = list[j];
+                    if ((u < v) == ((i & span) == 0)) {
+                        list[i] = v;
+                        list[j] = u;
                     }
+                }
+            }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            rank[j] = 2 * tid + j;
+            x[j] = rank[j] < n ? list[rank[j]] : 0;
+            if (rank[j] < n && (f.k == 0 || rank[j] < (uint32_t)f.k))
+                m[j] = mass_of(f, value_of((uint32_t)(x[j] >> 32)));
+        }
+        before[0] = block_before(m[0] + m[1], all, sh);
+        before[1] = before[0] + m[0];
+    }
     if (!row_mass) whole = (double)all;
     const double target = (double)f.top_p * whole;
     if (!whole_list && row_mass && (double)all < target) return {0, false};
