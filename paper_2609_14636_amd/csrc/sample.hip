@@ -148,23 +148,6 @@ __device__ __forceinline__ uint64_t block_max(uint64_t x, Shared &sh) {
     for (int i = 1; i < kWaves; ++i) x = sh.wave64[i] > x ? sh.wave64[i] : x;
     return x;
 }
-// The same with a float's maximum beside it.
-__device__ __forceinline__ uint64_t block_max(uint64_t x, float &y, Shared &sh) {
-    x = wave_max(x);
-    y = wave_max(y);
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) {
-        sh.wave64[threadIdx.x / kWave] = x;
-        sh.wavef[threadIdx.x / kWave].x = y;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        x = sh.wave64[i] > x ? sh.wave64[i] : x;
-        y = fmaxf(y, sh.wavef[i].x);
-    }
-    return x;
-}
 // The largest of two values at once.
 __device__ __forceinline__ float2 block_max2(float x, float y, Shared &sh) {
     float2 r = make_float2(wave_max(x), wave_max(y));
@@ -346,14 +329,46 @@ __device__ __attribute__((noinline)) Found first_entry(const Row<DT> row, Shared
 // s - log noise of one entry, in units of log 2 (s2 = s log2 e).
 __device__ __forceinline__ float race(float s2, float noise) { return s2 - lg2_all(noise); }
 
-// Keys of unfiltered rows are relative to the largest of the first entries, which the pass does not have to look for: near
-// the row's largest, so that a key's rounding is that of a small number.  Where it is not (the first entries masked by
-// large values, a small T), keys come out of it with fewer bits than the noise needs, and a second pass takes them
-// relative to the largest entry; also where the winner's noise may be subnormal.  Up to kFar, in units of log 2, the rounding is 2^-24 kFar = 4e-6 at most.
-constexpr float kFar = 64.0f;
-__device__ __forceinline__ bool not_settled(uint64_t best, float top, float ref, float c) {
-    return top > -INFINITY && (!(fabsf(top - ref) * c <= kFar) || (uint32_t)(best >> 32) == ordered(INFINITY));
-}
+// The winner among entries as they come, unfiltered.  Keys are relative to `ref`, one of the thread's own entries, which
+// moves up when a later one passes it by more than kFar (in units of log 2): a key's rounding is that of a number of that
+// size, 4e-6 at most, whatever is masked by large values before or after and at any temperature.
+constexpr float kFar = 32.0f;
+template <int DT>
+struct Race {
+    static constexpr int E = Elem<DT>::n;
+    float ref = -INFINITY, top = -INFINITY;
+    int at = -1;
+    __device__ __forceinline__ void add(const float *x, const u32x4 *noise, int i, float c) {
+        float m = x[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) m = fmaxf(m, x[e]);
+        if ((m - ref) * c > kFar) {
+            if (top < INFINITY) top += (ref - m) * c;
+            ref = m;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            // no key above -inf for an entry of -inf, whatever its noise
+            const float key = __builtin_fmaf(x[e] - ref, c, -lg2(__uint_as_float(noise[e / 4][e % 4])));
+            if (key > top) {
+                top = key;
+                at = i + e;
+            }
+        }
+    }
+    // Over the wave: every lane has the winner (0: none) and what it is relative to.
+    __device__ __forceinline__ uint64_t of_wave(float c, float &wave_ref) const {
+        wave_ref = wave_max(at < 0 ? -INFINITY : ref);
+        return wave_max(moved_to(at < 0 ? (uint64_t)0 : entry(top, at), ref, wave_ref, c));
+    }
+    // A winner relative to `from` as one relative to `to`.
+    static __device__ __forceinline__ uint64_t moved_to(uint64_t x, float from, float to, float c) {
+        const float key = value_of((uint32_t)(x >> 32));
+        return x == 0 || key == INFINITY ? x : (uint64_t)ordered(key + (from - to) * c) << 32 | (uint32_t)x;
+    }
+};
+// An infinite key: the winner's noise is 0 or below the normal range, and the row is passed again with its logarithm.
+__device__ __forceinline__ bool infinite(uint64_t best) { return (uint32_t)(best >> 32) == ordered(INFINITY); }
 
 // The largest key, relative to `ref`, of this thread's words among [begin, end), with its index (0: none).
 template <int DT, int Threads>
@@ -700,56 +715,49 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
     __syncthreads();
     Largest<DT> largest;
     if (temp == 0.0f || plain) {
-        float top = -INFINITY, ref = 0.0f;
-        int at = -1;
-        if (temp > 0.0f) {
-            // the point that keys are relative to: the largest of the part's first entries
-            largest.add(held[0]);
-            const float m = wave_max(largest.bad() ? -INFINITY : largest.value());
-            if (lane == 0) s_ends[wave].x = m;
-            __syncthreads();
-            ref = s_ends[0].x;
-#pragma unroll
-            for (int i = 1; i < kPartWaves; ++i) ref = fmaxf(ref, s_ends[i].x);
-            if (!(fabsf(ref) < INFINITY)) ref = 0.0f;
-        }
+        Race<DT> race;
         const u32x4 *nw = reinterpret_cast<const u32x4 *>(noise);
         each([&](const u32x4 &w, int i) __attribute__((always_inline)) {
             float x[E];
             widen<DT>(w, x);
             largest.add(w);
-            u32x4 q[E / 4];
+            if (temp > 0.0f) {
+                u32x4 q[E / 4];
 #pragma unroll
-            for (int j = 0; j < E / 4; ++j) {
-                q[j] = u32x4{};
-                if (temp > 0.0f && i + 4 * j < a.vocab) q[j] = __builtin_nontemporal_load(nw + i / 4 + j);
-            }
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float key = temp > 0.0f ? __builtin_fmaf(x[e] - ref, f.c, -lg2(__uint_as_float(q[e / 4][e % 4]))) : x[e];
-                if (key > top) {
-                    top = key;
-                    at = i + e;
+                for (int j = 0; j < E / 4; ++j) {
+                    q[j] = u32x4{};
+                    if (i + 4 * j < a.vocab) q[j] = __builtin_nontemporal_load(nw + i / 4 + j);
                 }
+                race.add(x, q, i, f.c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (x[e] > race.top) {
+                        race.top = x[e];
+                        race.at = i + e;
+                    }
             }
         });
-        const uint64_t m = wave_max(at < 0 ? (uint64_t)0 : entry(top, at));
-        const float wm = wave_max(largest.value());
+        float ref = 0.0f;
+        uint64_t m;
+        if (temp > 0.0f) m = race.of_wave(f.c, ref);
+        else m = wave_max(race.at < 0 ? (uint64_t)0 : entry(race.top, race.at));
         if (lane == 0) {
             s_best[wave] = m;
-            s_ends[wave].y = wm;
+            s_ends[wave].x = ref;
         }
         if (largest.bad()) s_bad = 1;
         __syncthreads();
-        uint64_t best = s_best[0];
-        float most = s_ends[0].y;
+        uint64_t best = 0;
+        ref = s_ends[0].x;
 #pragma unroll
-        for (int i = 1; i < kPartWaves; ++i) {
-            best = s_best[i] > best ? s_best[i] : best;
-            most = fmaxf(most, s_ends[i].y);
+        for (int i = 1; i < kPartWaves; ++i) ref = fmaxf(ref, s_ends[i].x);
+#pragma unroll
+        for (int i = 0; i < kPartWaves; ++i) {
+            const uint64_t y = temp > 0.0f ? Race<DT>::moved_to(s_best[i], s_ends[i].x, ref, f.c) : s_best[i];
+            best = y > best ? y : best;
         }
-        if (temp > 0.0f && !s_bad && not_settled(best, most, ref, f.c)) {  // the same for the whole workgroup
-            ref = most;
+        if (temp > 0.0f && infinite(best)) {  // the same for the whole workgroup
             const uint64_t again = wave_max(race_again<DT, kPartThreads>(row, noise, f.c, ref, begin, end));
             __syncthreads();
             if (lane == 0) s_best[wave] = again;
@@ -964,12 +972,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         best = x.best;
         bad = x.yes;
     } else if (plain) {
-        Largest<DT> first;
-        first.add(row.masked(row.load(tid), tid));
-        float ref = block_max2(first.bad() ? -INFINITY : first.value(), 0.0f, sh).x;
-        if (!(fabsf(ref) < INFINITY)) ref = 0.0f;
-        float top = -INFINITY;
-        int at = -1;
+        Race<DT> race;
         const u32x4 *nw = reinterpret_cast<const u32x4 *>(noise);
         const int words = (a.vocab + E - 1) / E;
         Largest<DT> seen;
@@ -993,21 +996,27 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
                 const u32x4 z = row.masked(w[u], i);
                 seen.add(z);
                 widen<DT>(z, x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    // no key above -inf for an entry of -inf, whatever its noise
-                    const float key = __builtin_fmaf(x[e] - ref, f.c, -lg2(__uint_as_float(q[u][e / 4][e % 4])));
-                    if (key > top) {
-                        top = key;
-                        at = i * E + e;
-                    }
-                }
+                race.add(x, q[u], i * E, f.c);
             }
         }
         bad |= seen.bad();
-        float most = seen.bad() ? -INFINITY : seen.value();
-        best = block_max(at < 0 ? (uint64_t)0 : entry(top, at), most, sh);
-        if (not_settled(best, most, ref, f.c)) best = block_max(race_again<DT, kThreads>(row, noise, f.c, most, 0, words), sh);
+        float ref;
+        best = race.of_wave(f.c, ref);
+        if ((tid & (kWave - 1)) == 0) {
+            sh.wave64[tid / kWave] = best;
+            sh.wavef[tid / kWave].x = ref;
+        }
+        __syncthreads();
+        ref = sh.wavef[0].x;
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) ref = fmaxf(ref, sh.wavef[i].x);
+        best = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            const uint64_t y = Race<DT>::moved_to(sh.wave64[i], sh.wavef[i].x, ref, f.c);
+            best = y > best ? y : best;
+        }
+        if (infinite(best)) best = block_max(race_again<DT, kThreads>(row, noise, f.c, ref, 0, words), sh);
     } else {
         // ---- first pass: every thread's maximum ----
         Largest<DT> largest;
