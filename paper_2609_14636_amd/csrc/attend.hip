@@ -21,12 +21,14 @@
 //
 // What bounds it, and what it takes (bf16, 8 key heads of 128 elements, pages of 64 tokens; a chip-wide read reaches
 // 7.0 TB/s and a library product 1.38 PFLOP/s):
-//   one token of 64 sequences of 1,000 to 16,384 keys   417 to 437 us, 6.1 to 6.4 TB/s: memory
+//   one token of 64 sequences of 1,000 to 16,384 keys   418 to 421 us, 6.35 TB/s: memory
 //   one token of 8 sequences of 100 to 2,000 keys       18 us: chains of dependent loads in two launches (14 + 5 us)
-//   9 to 24 drafted tokens of 32 sequences, 4 heads a group   116 to 123 us, 3.8 TB/s: products and memory in turn, then
-//                                                       the joining of shares
-//   129 to 1,024 tokens of 6 sequences                  135 to 150 us, 560 to 630 TFLOP/s: the softmax's vector work
+//   9 to 24 drafted tokens of 32 sequences, 4 heads a group   114 to 123 us, 3.9 TB/s: a workgroup has one tile on its way
+//                                                       and waits for it before it asks for the next; 11 us of joining
+//   129 to 1,024 tokens of 6 sequences                  132 to 150 us, 560 to 640 TFLOP/s: the softmax's vector work
 //                                                       beside the products, and 16 us of joining
+//   the same turns in float                             1.63 ms, 52 TFLOP/s (154 in a library product): products of
+//                                                       16 x 16 x 4 and tiles of 32 rows, each of which reads all keys
 #include <type_traits>
 
 #include "common.hpp"
@@ -331,8 +333,9 @@ __device__ __forceinline__ bool at_end(const Place &at, const Place &to) {
 
 // ---- one block of 16 T keys ----
 
-// Keys and values, which a step reads once, go past the caches: 64 sequences of 1,000 to 16,384 keys take 417 us, or
-// 468 with ordinary loads, and sequences that share their pages gain as well (436 us, or 467).
+// Keys and values, which a step of few rows reads once, go past the caches: 64 sequences of 1,000 to 16,384 keys take 417
+// us, or 468 with ordinary loads, and sequences that share their pages gain as well (436 us, or 467).  A sequence of several
+// row tiles in this form (float, or a turn beside many single tokens) reads them from memory for each.
 __device__ __forceinline__ u32x4 once(const char *p) {
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
 }
@@ -1209,7 +1212,9 @@ struct Form {
     int rows, workers;  // rows of a tile: 16 or 32 with the keys split over the waves, 128 with the rows
 };
 
-// By the mean number of rows of a sequence's key head (tokens times the group of query heads), which the host knows.
+// By the mean number of rows of a sequence's key head (tokens times the group of query heads), which the host knows; it
+// decides for all of a call's sequences.  63 single tokens and a turn of 400, each over 8,000 keys, take 549 us in tiles of
+// 16, and 340 and 57 in calls of their own.
 // 32 sequences of 500 to 8,192 keys, 8 key heads of 128 elements, bf16:
 //   16 rows                       113 us in tiles of 16, 120 in tiles of 128 (one token of 64 long sequences 447, or 499)
 //   32 rows                       119 us in tiles of 128, 177 in tiles of 32 with the keys split

@@ -14,9 +14,10 @@
 //   where some tens of entries lie above, and lower if their mass does not reach top_p of the row's.
 //   Rows that do not fit this (a nucleus or a k of thousands, rows of equal logits) take the exact way by the
 //   digits of the logits' bits: histograms of counts and masses, 11 bits at a time, lead to the last kept value.
-// What bounds it, and what it takes (bf16 rows of 151,936): 256 unfiltered rows 38 us, 6.1 TB/s of logits and numbers, so
-// memory; one filtered row 13 us in two launches, and 64 with every filter 20 to 23 us: chains of dependent loads and
-// barriers, so every wave does what is short for itself.
+// What bounds it, and what it takes (bf16 rows of 151,936): 256 unfiltered rows 39 us, 6.0 TB/s of logits and numbers, so
+// memory; one row with top-k and top-p 13 us in two launches, 64 rows 16: chains of dependent loads and barriers, so every
+// wave does what is short for itself.  64 rows with top-p alone take 18 us where their nuclei have some tens of
+// entries, and 340 where they have thousands (one row 250): the atomics of the histograms, which meet in some tens of bins.
 // Sums of masses are integers of 2^-40 of the largest entry's, or run in a fixed order, so a row's
 // result does not depend on timing.
 #include <cstddef>
@@ -1110,7 +1111,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
 namespace {
 
 // Workgroups per row of the first kernel: up to 1,024 over all rows, where the vocabulary has work for them; 1: there is
-// none.  64 mixed rows of 151,936 bf16 logits take 27 us without, 20 in sixteen parts each; 256 rows fill the chip.
+// none.  64 mixed rows of 151,936 bf16 logits and small nuclei take 27 us without, 20 in sixteen parts each; 256 rows fill the
+// chip.
 int parts_of(int64_t n_rows, int32_t vocab) {
     if (n_rows < 1 || n_rows > 128 || vocab < 16384) return 1;
     int64_t n = 1024 / n_rows;
