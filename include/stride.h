@@ -310,8 +310,8 @@ stride_status stride_records_plan(stride_records *rec, int32_t n_tasks, const in
                                   int32_t *k_max);
 
 /*
- * Paged cache of keys and values, the memory of rollouts being generated: the rollout that restarts from
- * its k0 leading units keeps those units' pages, and rollouts of one task may name the same pages for
+ * Paged cache of keys and values, the memory of rollouts being generated: a rollout that restarts from
+ * its k0 leading units can keep those units' pages, and rollouts of one task may name the same pages for
  * what they have in common.
  *
  * Token `slot` of sequence s (its place in the sequence, from 0) is in slot % page_size of page
@@ -323,7 +323,7 @@ stride_status stride_records_plan(stride_records *rec, int32_t n_tasks, const in
  *   dtype         STRIDE_BF16 or STRIDE_F32, also of queries and outputs
  *   head_dim      64, 96, 128 or 256
  *   page_size     a power of two up to 65536
- *   page_table    device int32 [n_seqs, max_pages], rows table_ld >= max_pages apart;
+ *   page_table    device int32 [n_seqs, max_pages], rows table_ld >= max_pages apart (they do not overlap);
  *                 max_pages * page_size is at most 2^31 - 256
  */
 typedef struct {
